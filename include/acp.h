@@ -456,9 +456,10 @@ acp_status acp_adamw_tensor_info(const acp_adamw *opt, int32_t tensor, int64_t *
  * whose gradients alternate between buffers (the compressor's factors swap roles with the step's
  * parity) sets a slot for each once and names it in every call.  The device block (256-byte aligned, of
  * acp_adamw_grads_bytes for the same entries) takes the launch tables and the norm's partial sums and
- * belongs to the slot until it is set again.  Uploads on `stream` and waits for it.  Factors may be
- * read-only views of a context's state (acp_factor_address).  ACP_E_INVALID if a gradient overlaps
- * what the calls write, or for more than about 2^33 elements (the launches' limit; take several optimisers).
+ * belongs to the slot until it is set again, or the state bound again; so do the gradients' places.  Uploads
+ * on `stream` and waits for it.  Factors may be read-only views of a context's state
+ * (acp_factor_address).  ACP_E_INVALID if a gradient overlaps what the calls write (the state, parameters and
+ * copies, any slot's block) or the block any of these or any slot's gradients, or for more than about 2^33 elements (the launches' limit; take several optimisers).
  */
 acp_status acp_adamw_grads_bytes(const acp_adamw *opt, const acp_adamw_grad *grads, int64_t *bytes);
 acp_status acp_adamw_set_grads(acp_adamw *opt, int32_t slot, const acp_adamw_grad *grads, void *device_ptr,
@@ -467,7 +468,8 @@ acp_status acp_adamw_set_grads(acp_adamw *opt, int32_t slot, const acp_adamw_gra
 /*
  * acp_adamw_norm - the 2-norm of `scale` times all gradients of a slot together, and the coefficient
  * that clips it: clip[0] = norm, clip[1] = min(1, max_norm / norm), NaN if the norm is not finite (clip:
- * device, two floats).  Sums are in fp64 in a fixed order.  A factored gradient's part is
+ * device, two floats; ACP_E_INVALID if they overlap the state, parameters, copies or a slot's block or
+ * gradients).  Sums are in fp64 in a fixed order.  A factored gradient's part is
  * sum (a^T a) o (b^T b).  max_norm > 0; infinity does not clip.
  */
 acp_status acp_adamw_norm(acp_adamw *opt, int32_t slot, float scale, float max_norm, float *clip, void *stream);
@@ -475,7 +477,8 @@ acp_status acp_adamw_norm(acp_adamw *opt, int32_t slot, float scale, float max_n
 /*
  * acp_adamw_step - step `step` (1, 2, ...; the caller counts) of every tensor with a slot's gradients.
  * lr >= 0, betas in [0, 1), eps >= 2^-126, weight_decay >= 0, all finite, else ACP_E_INVALID.
- * `clip` (device, from acp_adamw_norm, or NULL): gradients are multiplied by clip[1] as well; where it is
+ * `clip` (device, from acp_adamw_norm, or NULL; outside what the call writes and the slots' blocks, else
+ * ACP_E_INVALID): gradients are multiplied by clip[1] as well; where it is
  * NaN the call changes nothing, parameters and moments included.
  */
 acp_status acp_adamw_step(acp_adamw *opt, int32_t slot, int64_t step, const acp_adamw_hyper *hyper,

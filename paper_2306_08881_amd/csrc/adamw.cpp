@@ -16,6 +16,15 @@ hipError_t adamw_launch_step(const AwSlotPlan& s, int bits, const AwArgs& a, hip
 hipError_t adamw_launch_norm(const AwSlotPlan& s, AwNormArgs a, hipStream_t st);
 }  // namespace acp
 
+namespace {
+
+struct Span {
+  uintptr_t first, last;
+  bool write;
+};
+
+}  // namespace
+
 struct acp_adamw {
   acp::AwPlan plan;
   uint8_t* dev = nullptr;   // bound state block
@@ -26,6 +35,9 @@ struct acp_adamw {
     uint8_t* dev = nullptr;  // the slot's gradient block
   };
   Slot slots[acp::kAwSlots];
+  // what the calls write (state, parameters, copies, the slots' blocks) and what they read (the slots'
+  // gradients), each sorted and without overlaps
+  std::vector<Span> written, read;
   mutable std::string err;
 };
 
@@ -61,11 +73,6 @@ acp_status check_device(const acp_adamw* o) {
   return ACP_OK;
 }
 
-struct Span {
-  uintptr_t first, last;
-  bool write;
-};
-
 // Whether any two spans meet of which one at least is written.
 bool clash(std::vector<Span>& v) {
   std::sort(v.begin(), v.end(), [](const Span& x, const Span& y) { return x.first < y.first; });
@@ -91,6 +98,38 @@ void state_spans(const acp_adamw* o, std::vector<Span>& v) {
     add(v, t.p, t.n * t.m * 4, true);
     add(v, t.copy, t.n * t.m * 2, true);
   }
+}
+
+// the spans of a slot's block and gradients
+void slot_spans(const acp_adamw* o, const acp::AwSlotPlan& s, const void* block, std::vector<Span>& v) {
+  add(v, block, s.total_bytes, true);
+  for (size_t i = 0; i < s.grads.size(); ++i) {
+    const acp::AwGrad& g = s.grads[i];
+    const acp::AwTensor& t = o->plan.tensors[i];
+    add(v, g.g, t.n * t.m * (g.bf16 ? 2 : 4), false);
+    add(v, g.a, t.n * g.rank * 4, false);
+    add(v, g.b, t.m * g.rank * 4, false);
+  }
+}
+
+// Those spans that are written, or only read, with overlapping and adjoining ones as one (v is sorted).
+std::vector<Span> merged(const std::vector<Span>& v, bool write) {
+  std::vector<Span> out;
+  for (const Span& s : v) {
+    if (s.write != write) continue;
+    if (!out.empty() && s.first <= out.back().last)
+      out.back().last = std::max(out.back().last, s.last);
+    else
+      out.push_back(s);
+  }
+  return out;
+}
+
+// Whether `bytes` from p on meet any of the spans (of merged()).
+bool meets(const std::vector<Span>& v, const void* p, int64_t bytes) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  const auto next = std::upper_bound(v.begin(), v.end(), a, [](uintptr_t x, const Span& s) { return x < s.first; });
+  return (next != v.end() && next->first < a + static_cast<uintptr_t>(bytes)) || (next != v.begin() && a < (next - 1)->last);
 }
 
 // the gradients' values and factors
@@ -174,6 +213,7 @@ acp_status acp_adamw_bind(acp_adamw* o, void* device_ptr, int64_t bytes, float* 
       add(spans, ts[i].copy, ts[i].n * ts[i].m * 2, true);
     }
     if (clash(spans)) return fail(o, ACP_E_INVALID, "parameters, copies and the state block overlap");
+    std::vector<Span> written = merged(spans, true);
     int dev = -1;
     if (hipGetDevice(&dev) != hipSuccess) return fail(o, ACP_E_DEVICE, "hipGetDevice failed");
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -186,6 +226,8 @@ acp_status acp_adamw_bind(acp_adamw* o, void* device_ptr, int64_t bytes, float* 
     if (e == hipSuccess) e = hipStreamSynchronize(s);
     if (e != hipSuccess) return fail(o, ACP_E_DEVICE, std::string("bind failed: ") + hipGetErrorString(e));
     o->plan.tensors.swap(ts);
+    o->written.swap(written);
+    o->read.clear();
     o->dev = d;
     o->device = dev;
     o->has_params = params != nullptr;
@@ -244,15 +286,12 @@ acp_status acp_adamw_set_grads(acp_adamw* o, int32_t slot, const acp_adamw_grad*
     if (bytes < s.total_bytes) return fail(o, ACP_E_STATE, "gradient block too small");
     std::vector<Span> spans;
     state_spans(o, spans);
-    add(spans, device_ptr, s.total_bytes, true);
-    for (size_t i = 0; i < s.grads.size(); ++i) {
-      const acp::AwGrad& g = s.grads[i];
-      const acp::AwTensor& t = o->plan.tensors[i];
-      add(spans, g.g, t.n * t.m * (g.bf16 ? 2 : 4), false);
-      add(spans, g.a, t.n * g.rank * 4, false);
-      add(spans, g.b, t.m * g.rank * 4, false);
-    }
-    if (clash(spans)) return fail(o, ACP_E_INVALID, "gradients overlap the parameters, the state or the gradient block");
+    slot_spans(o, s, device_ptr, spans);
+    for (int32_t i = 0; i < acp::kAwSlots; ++i)
+      if (i != slot && o->slots[i].dev) slot_spans(o, o->slots[i].plan, o->slots[i].dev, spans);
+    if (clash(spans))
+      return fail(o, ACP_E_INVALID, "gradients or the gradient block overlap the parameters, the state or another slot's");
+    std::vector<Span> written = merged(spans, true), read = merged(spans, false);
     if ((st = check_device(o)) != ACP_OK) return st;
     hipStream_t sm = static_cast<hipStream_t>(stream);
     uint8_t* d = static_cast<uint8_t*>(device_ptr);
@@ -265,6 +304,8 @@ acp_status acp_adamw_set_grads(acp_adamw* o, int32_t slot, const acp_adamw_grad*
     s.tiles = {};  // the device has them
     o->slots[slot].plan = std::move(s);
     o->slots[slot].dev = d;
+    o->written.swap(written);
+    o->read.swap(read);
     o->err.clear();
     return ACP_OK;
   });
@@ -276,6 +317,8 @@ acp_status acp_adamw_norm(acp_adamw* o, int32_t slot, float scale, float max_nor
     const acp_status st = check_slot(o, slot);
     if (st != ACP_OK) return st;
     if (!clip || !aligned(clip, 4)) return fail(o, ACP_E_INVALID, "clip must be a device buffer of two floats");
+    if (meets(o->written, clip, 8) || meets(o->read, clip, 8))
+      return fail(o, ACP_E_INVALID, "clip overlaps the parameters, the state or a slot's block or gradients");
     if (!std::isfinite(scale)) return fail(o, ACP_E_INVALID, "scale must be finite");
     if (!(max_norm > 0.f)) return fail(o, ACP_E_INVALID, "max_norm must be positive (infinity does not clip)");
     const acp_adamw::Slot& s = o->slots[slot];
@@ -312,6 +355,8 @@ acp_status acp_adamw_step(acp_adamw* o, int32_t slot, int64_t step, const acp_ad
       return fail(o, ACP_E_INVALID, "weight_decay must be finite and not negative");
     if (!std::isfinite(h->scale)) return fail(o, ACP_E_INVALID, "scale must be finite");
     if (!aligned(clip, 4)) return fail(o, ACP_E_INVALID, "misaligned clip");
+    if (clip && meets(o->written, clip, 8))
+      return fail(o, ACP_E_INVALID, "clip overlaps the parameters, the state or a slot's block");
     const acp_adamw::Slot& s = o->slots[slot];
     acp::AwArgs a{};
     a.tensors = reinterpret_cast<const acp::AwTensor*>(o->dev + o->plan.off_tensors);
