@@ -3,6 +3,10 @@
 ``AdamW`` owns one ``acp_adamw``, the device block of its moments and a gradient block per slot (torch
 uint8 tensors); its methods carry the C names without the ``acp_adamw_`` prefix and pass torch device
 pointers and the current HIP stream through.
+
+The optimiser's own memory comes from the stream of the call that makes it (``bind``, ``set_grads``, which
+wait for that stream), and stays until what other streams were given on it has ended.  Work on several streams
+is put in order by the caller; a stream that the caller made by other means than torch outlives the optimiser.
 """
 
 from __future__ import annotations
@@ -66,6 +70,7 @@ class AdamW:
         self.state, self.clip = None, None
         self.params, self.copies = None, None
         self._grads: Dict[int, tuple] = {}
+        self._streams: Dict[int, object] = {}  # that calls were made on, by address
         self.bind(params, copies, device, stream)
 
     def _check(self, status: int, where: str):
@@ -73,7 +78,17 @@ class AdamW:
             raise L.AcpError(status, where, self.lib.acp_adamw_last_error(self.opt).decode())
 
     def _stream(self, stream) -> int:
-        return _current_stream(self.device.index) if stream is None else stream.cuda_stream
+        s = _current_stream(self.device.index) if stream is None else stream.cuda_stream
+        if s not in self._streams and self.state is not None:
+            self._streams[s] = torch.cuda.current_stream(self.device) if stream is None else stream
+            self._record(self.state, self.clip, *(block for _, block in self._grads.values()))
+        return s
+
+    def _record(self, *tensors):
+        """The memory of these is not given to others before what the streams have on it has ended."""
+        for t in tensors:
+            for s in self._streams.values():
+                t.record_stream(s)
 
     def _clip(self, clip) -> int:
         return self._clip_ptr if clip is self.clip else _ptr(clip, (torch.float32,), 2, "clip")
@@ -101,13 +116,15 @@ class AdamW:
                                             for t, k in zip(ts, self.numels)])
 
         p, c = addresses(params, torch.float32, "parameter"), addresses(copies, torch.bfloat16, "copy")
-        with torch.cuda.device(self.device):
+        on = torch.cuda.current_stream(self.device) if stream is None else stream
+        with torch.cuda.stream(on), torch.cuda.device(self.device):
             nbytes = self.state_bytes()
+            clip = torch.zeros(2, device=self.device)
             state = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-            self._check(self.lib.acp_adamw_bind(self.opt, state.data_ptr(), nbytes, p, c, self._stream(stream)),
+            self._check(self.lib.acp_adamw_bind(self.opt, state.data_ptr(), nbytes, p, c, on.cuda_stream),
                         "acp_adamw_bind")
-            self.clip = torch.zeros(2, device=self.device)
-            self._clip_ptr = self.clip.data_ptr()
+        self._record(state, clip)
+        self.clip, self._clip_ptr = clip, clip.data_ptr()
         self.state, self.params, self.copies = state, params, copies
         self._grads = {}
 
@@ -152,10 +169,12 @@ class AdamW:
                 x.type = L.ACP_GRAD_BF16 if g.dtype == torch.bfloat16 else L.ACP_GRAD_FP32
         v = C.c_int64()
         self._check(self.lib.acp_adamw_grads_bytes(self.opt, arr, C.byref(v)), "acp_adamw_grads_bytes")
-        with torch.cuda.device(self.device):
+        on = torch.cuda.current_stream(self.device) if stream is None else stream
+        with torch.cuda.stream(on), torch.cuda.device(self.device):
             block = torch.empty(v.value, dtype=torch.uint8, device=self.device)
-            self._check(self.lib.acp_adamw_set_grads(self.opt, slot, arr, block.data_ptr(), v.value, self._stream(stream)),
+            self._check(self.lib.acp_adamw_set_grads(self.opt, slot, arr, block.data_ptr(), v.value, on.cuda_stream),
                         "acp_adamw_set_grads")
+        self._record(block)
         self._grads[slot] = (list(grads), block)
 
     # ---- the step
