@@ -69,11 +69,14 @@ class Acp:
     def bind_state(self, device=None, stream=None):
         import torch
         dev = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-        with torch.cuda.device(dev):
+        on = torch.cuda.current_stream(dev) if stream is None else stream
+        # memory of the stream that clears and fills it, which acp_bind_state waits for
+        with torch.cuda.stream(on), torch.cuda.device(dev):
             nbytes = self.state_bytes()
-            self.state = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-            _check(self.lib.acp_bind_state(self.ctx, self.state.data_ptr(), nbytes, _stream_ptr(stream)),
-                   self.lib, self.ctx, "acp_bind_state")
+            state = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+            _check(self.lib.acp_bind_state(self.ctx, state.data_ptr(), nbytes, on.cuda_stream), self.lib, self.ctx,
+                   "acp_bind_state")
+        self.state = state
 
     # ---- layout
     def num_buckets(self) -> int:
