@@ -141,7 +141,8 @@ __device__ inline bool grad_factor(const AwArgs& a, float& c) {
 }
 
 // sqrt(x) correctly rounded for x >= 2^-100: the instruction's result (1 ulp), or the neighbour beside
-// which the residual x - s s' says the root lies.  0, infinity and NaN fail both tests and stay.
+// which the residual x - s s' says the root lies.  Below, where fp32 does not hold all residuals, within 2 ulp;
+// subnormal x the instruction takes for 0.  0, infinity and NaN fail both tests and stay.
 __device__ inline float root(float x) {
   const float s = __builtin_amdgcn_sqrtf(x);
   const float lo = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, s) - 1u);
@@ -150,19 +151,34 @@ __device__ inline float root(float x) {
   return above > 0.f ? hi : below <= 0.f ? lo : s;
 }
 
-// m, v and p updated in place; returns sqrt(v').  What goes into the moments is rounded operation by
-// operation, as anyone would write it: 8-bit moments turn a difference in the last bit into one of a
+// m, v and p of a lane's four elements updated in place; r: sqrt(v').  What goes into the moments is rounded
+// operation by operation, as anyone would write it: 8-bit moments turn a difference in the last bit into one of a
 // whole code now and then, which another program's replay of the step would see (fused and with the bare
 // instruction for the root: BERT-large rank 32 937 us, so 944).  p's quotient is m' times the hardware's
 // reciprocal (1 ulp; eps > 0 keeps the denominator a normal number, and an infinite one gives 0).
-__device__ inline float update1(const AwArgs& a, const Coef& k, float g, float& p, float& m, float& v) {
-  g = g * k.c;
-  m = m * a.b1 + g * a.c1;
-  v = v * a.b2 + (g * g) * a.c2;
-  const float r = root(v);
-  const float den = __builtin_fmaf(r, a.rs, a.eps);
-  p = __builtin_fmaf(-(m * __builtin_amdgcn_rcpf(den)), a.lr, p * k.decay);
-  return r;
+// Subnormal v' are scaled for their roots, in waves that have any (BERT-large rank 32, 8 bits, 941 us without,
+// 949 so; 960 with every element scaled or not by a select, and BERT-base 340, 346 and 342).
+constexpr int kSubnormal = 0x80;  // class of positive subnormal numbers
+__device__ inline void update4(const AwArgs& a, const Coef& k, const float (&g)[4], float (&p)[4], float (&m)[4],
+                               float (&v)[4], float (&r)[4]) {
+  bool tiny = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float c = g[i] * k.c;
+    m[i] = m[i] * a.b1 + c * a.c1;
+    v[i] = v[i] * a.b2 + (c * c) * a.c2;
+    r[i] = root(v[i]);
+    tiny = tiny || __builtin_amdgcn_classf(v[i], kSubnormal);
+  }
+  if (__builtin_expect(__any(tiny), 0)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = v[i] < 0x1p-126f ? root(v[i] * 0x1p64f) * 0x1p-32f : r[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float den = __builtin_fmaf(r[i], a.rs, a.eps);
+    p[i] = __builtin_fmaf(-(m[i] * __builtin_amdgcn_rcpf(den)), a.lr, p[i] * k.decay);
+  }
 }
 
 // ---- 8-bit moments -----------------------------------------------------------------------------
@@ -317,22 +333,22 @@ template <int BITS, bool WIDE>
 __device__ inline void step_lane(const AwArgs& a, const AwTensor& t, const Coef& k, uint32_t e0, const Streams& s,
                                  uint32_t at, int len, uint32_t blk, Lane<BITS>& x, const float (&g)[4]) {
   if constexpr (BITS == 32) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) update1(a, k, g[i], x.p[i], x.m[i], x.v[i]);
+    float r[4];
+    update4(a, k, g, x.p, x.m, x.v, r);
     st4(s.p, at, x.p);
     st4(s.m, at, x.m);
     st4(s.v, at, x.v);
   } else {
-    float m[4], r[4];
+    float m[4], v[4], r[4];
     values_of(x.m, m);
     values_of(x.v, r);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       m[i] = m[i] * x.ms;
       r[i] = r[i] * x.vs;
-      float v = r[i] * r[i];
-      r[i] = update1(a, k, g[i], x.p[i], m[i], v);
+      v[i] = r[i] * r[i];
     }
+    update4(a, k, g, x.p, m, v, r);
     // elements past the end have zeros, or NaN beside a dead block's others
     const Scales sc = block_scales(wave_max(top4(m)), wave_max(top4(r)));
     uint32_t cm = 0, cr = 0;
