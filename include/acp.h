@@ -476,7 +476,9 @@ acp_status acp_adamw_norm(acp_adamw *opt, int32_t slot, float scale, float max_n
 
 /*
  * acp_adamw_step - step `step` (1, 2, ...; the caller counts) of every tensor with a slot's gradients.
- * lr >= 0, betas in [0, 1), eps >= 2^-126, weight_decay >= 0, all finite, else ACP_E_INVALID.
+ * lr >= 0, betas in [0, 1), eps from 2^-126 to 2^126, weight_decay >= 0, all finite, else ACP_E_INVALID;
+ * and so where a value is not as the kernels have it in fp32: betas round below 1 (1 - 2^-25 does not), and
+ * lr / (1 - b1^t) and 1 - lr * weight_decay are finite.
  * `clip` (device, from acp_adamw_norm, or NULL; outside what the call writes and the slots' blocks, else
  * ACP_E_INVALID): gradients are multiplied by clip[1] as well; where it is
  * NaN the call changes nothing, parameters and moments included.

@@ -347,26 +347,10 @@ acp_status acp_adamw_step(acp_adamw* o, int32_t slot, int64_t step, const acp_ad
     if (step < 1) return fail(o, ACP_E_STEP, "steps count from 1");
     if (!h) return fail(o, ACP_E_INVALID, "null hyperparameters");
     if (!(std::isfinite(h->lr) && h->lr >= 0.0)) return fail(o, ACP_E_INVALID, "lr must be finite and not negative");
-    if (!(h->beta1 >= 0.0 && h->beta1 < 1.0) || !(h->beta2 >= 0.0 && h->beta2 < 1.0))
-      return fail(o, ACP_E_INVALID, "betas must be in [0, 1)");
-    if (!(std::isfinite(h->eps) && static_cast<float>(h->eps) >= 0x1p-126f))
-      return fail(o, ACP_E_INVALID, "eps must be a positive normal number");
     if (!(std::isfinite(h->weight_decay) && h->weight_decay >= 0.0))
       return fail(o, ACP_E_INVALID, "weight_decay must be finite and not negative");
     if (!std::isfinite(h->scale)) return fail(o, ACP_E_INVALID, "scale must be finite");
-    if (!aligned(clip, 4)) return fail(o, ACP_E_INVALID, "misaligned clip");
-    if (clip && meets(o->written, clip, 8))
-      return fail(o, ACP_E_INVALID, "clip overlaps the parameters, the state or a slot's block");
-    const acp_adamw::Slot& s = o->slots[slot];
     acp::AwArgs a{};
-    a.tensors = reinterpret_cast<const acp::AwTensor*>(o->dev + o->plan.off_tensors);
-    a.grads = reinterpret_cast<const acp::AwGrad*>(s.dev + s.plan.off_grads);
-    a.tiles = reinterpret_cast<const acp::AwTile*>(s.dev + s.plan.off_tiles);
-    a.m = o->dev + o->plan.off_m;
-    a.v = o->dev + o->plan.off_v;
-    a.ms = reinterpret_cast<float*>(o->dev + o->plan.off_ms);
-    a.vs = reinterpret_cast<float*>(o->dev + o->plan.off_vs);
-    a.clip = clip;
     const double t = static_cast<double>(step);
     a.b1 = static_cast<float>(h->beta1);
     a.c1 = static_cast<float>(1.0 - h->beta1);
@@ -377,6 +361,25 @@ acp_status acp_adamw_step(acp_adamw* o, int32_t slot, int64_t step, const acp_ad
     a.eps = static_cast<float>(h->eps);
     a.decay = static_cast<float>(1.0 - h->lr * h->weight_decay);
     a.scale = h->scale;
+    // as the kernels have them: a beta that fp32 takes for 1 would never let its moment fall
+    if (!(h->beta1 >= 0.0 && a.b1 < 1.f) || !(h->beta2 >= 0.0 && a.b2 < 1.f))
+      return fail(o, ACP_E_INVALID, "betas must be in [0, 1) and stay below 1 in fp32");
+    // (above 2^126 the reciprocal of the update's denominator would be subnormal)
+    if (!(a.eps >= 0x1p-126f && a.eps <= 0x1p126f)) return fail(o, ACP_E_INVALID, "eps must be from 2^-126 to 2^126");
+    if (!std::isfinite(a.lr)) return fail(o, ACP_E_INVALID, "lr with its bias correction must be finite in fp32");
+    if (!std::isfinite(a.decay)) return fail(o, ACP_E_INVALID, "lr times weight_decay must be finite in fp32");
+    if (!aligned(clip, 4)) return fail(o, ACP_E_INVALID, "misaligned clip");
+    if (clip && meets(o->written, clip, 8))
+      return fail(o, ACP_E_INVALID, "clip overlaps the parameters, the state or a slot's block");
+    const acp_adamw::Slot& s = o->slots[slot];
+    a.tensors = reinterpret_cast<const acp::AwTensor*>(o->dev + o->plan.off_tensors);
+    a.grads = reinterpret_cast<const acp::AwGrad*>(s.dev + s.plan.off_grads);
+    a.tiles = reinterpret_cast<const acp::AwTile*>(s.dev + s.plan.off_tiles);
+    a.m = o->dev + o->plan.off_m;
+    a.v = o->dev + o->plan.off_v;
+    a.ms = reinterpret_cast<float*>(o->dev + o->plan.off_ms);
+    a.vs = reinterpret_cast<float*>(o->dev + o->plan.off_vs);
+    a.clip = clip;
     a.key = acp::adamw_step_key(o->plan.seed, step);
     const hipError_t e = acp::adamw_launch_step(s.plan, o->plan.bits, a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(o, ACP_E_DEVICE, std::string("kernel launch failed: ") + hipGetErrorString(e));
