@@ -398,8 +398,8 @@ void acp_destroy(acp_ctx *ctx);
  * acp_adamw_norm and acp_adamw_step enqueue kernels only and may be captured into a HIP graph, with the
  * arguments of the call (a replay repeats its step's lr and bias corrections).  Pointers need the
  * alignment of their type.  A factored gradient has at most 2^24 columns and 2^30 rows
- * (ACP_E_UNSUPPORTED).  An acp_adamw is not thread-safe; calls on one acp_adamw that run on several
- * streams must be ordered by the caller.
+ * (ACP_E_UNSUPPORTED; acp_adamw_set_grads says how much a slot takes).  An acp_adamw is not thread-safe; calls
+ * on one acp_adamw that run on several streams must be ordered by the caller.
  */
 typedef struct acp_adamw acp_adamw;
 
@@ -459,7 +459,12 @@ acp_status acp_adamw_tensor_info(const acp_adamw *opt, int32_t tensor, int64_t *
  * belongs to the slot until it is set again, or the state bound again; so do the gradients' places.  Uploads
  * on `stream` and waits for it.  Factors may be read-only views of a context's state
  * (acp_factor_address).  ACP_E_INVALID if a gradient overlaps what the calls write (the state, parameters and
- * copies, any slot's block) or the block any of these or any slot's gradients, or for more than about 2^33 elements (the launches' limit; take several optimisers).
+ * copies, any slot's block) or the block any of these or any slot's gradients; also, from acp_adamw_grads_bytes
+ * on, for 2^22 tiles of a kind or more (the launches' limit; take several optimisers).  A tile is, of a
+ * gradient of values, 2048 elements (32 bits) or 16 blocks (8 bits); of factors, 16 rows of a column of blocks
+ * or more (rows of 256 columns and more), or as many whole blocks as 16 rows hold, at least one (shorter
+ * rows); for the norm, 16384 values, or 256 rows of a factor (above rank 64 1024, for each pair of its 64-column
+ * parts).  Above rank 128 both kinds of the steps on factors together stay below 2^23.
  */
 acp_status acp_adamw_grads_bytes(const acp_adamw *opt, const acp_adamw_grad *grads, int64_t *bytes);
 acp_status acp_adamw_set_grads(acp_adamw *opt, int32_t slot, const acp_adamw_grad *grads, void *device_ptr,

@@ -457,10 +457,7 @@ __global__ __launch_bounds__(dense_threads<WIDE>()) void k_adamw(AwArgs a) {
 
 // ---- step on gradients given as factors --------------------------------------------------------
 
-// Waves of a workgroup that share a tile's columns: four, which meet at fewer barriers (8 bits, BERT-large
-// rank 32 959 us, with eight 1036), but eight above rank 128, where B's part would leave a SIMD one wave (rank
-// 256 2701 us, with eight 2495).
-constexpr int product_group(int kc) { return kc <= 8 ? 4 : 8; }
+constexpr int product_group(int kc) { return aw_product_waves(16 * kc); }
 
 // The operands of a product for 16 rows of A or B, 16 KC values of the inner dimension, row l of a factor's
 // rows in `r` from value `row` on: lane 16 q + l has the values 4 q .. 4 q + 3 of each 16, or below rank 16 the
@@ -946,6 +943,7 @@ void launch_dense(int64_t tiles, const AwArgs& a, hipStream_t st) {
 template <int BITS, int KC, bool WIDE>
 void launch_products(int64_t tiles, int64_t narrow, int64_t joined, AwArgs a, hipStream_t st) {
   constexpr int W = product_group(KC);
+  static_assert(dense_groups<BITS, false>(W) == aw_joined_groups(BITS, W), "the planner counts a launch's threads");
   a.count = static_cast<uint32_t>(tiles);
   a.narrow = static_cast<uint32_t>(narrow);
   a.joined = static_cast<uint32_t>(joined);

@@ -44,6 +44,13 @@ constexpr int64_t kAwProductTiles = 4096;
 // model, or what else a launch of its own, 5 us, would cost more than their lower occupancy there)
 constexpr int64_t kAwJoined = int64_t(1) << 21;
 
+// Waves of a workgroup of A B^T that share a tile's columns: four, which meet at fewer barriers (8 bits, BERT-large
+// rank 32 959 us, with eight 1036), but eight above rank 128, where B's part would leave a SIMD one wave (rank
+// 256 2701 us, with eight 2495).
+constexpr int aw_product_waves(int rank) { return rank <= 128 ? 4 : 8; }
+// Workgroups of `waves` waves that share a joined dense tile, a wave taking kAwPart elements or one block.
+constexpr int64_t aw_joined_groups(int bits, int64_t waves) { return (bits == 32 ? kAwTile / kAwPart : kAwTileBlocks) / waves; }
+
 struct AwTensor {
   float* p;       // parameters
   uint16_t* copy; // bfloat16 copy, or null
