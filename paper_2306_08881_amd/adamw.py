@@ -23,9 +23,11 @@ _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _ptr(t, dtypes, numel: int, what: str) -> int:
+def _ptr(t, dtypes, numel: int, what: str, device) -> int:
     if t.dtype not in dtypes or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous device tensor of {' or '.join(str(d) for d in dtypes)}")
+    if t.device != device:
+        raise ValueError(f"{what}: expected a tensor on {device}, got one on {t.device}")
     if t.numel() != numel:
         raise ValueError(f"{what}: expected {numel} elements, got {t.numel()}")
     return t.data_ptr()
@@ -91,7 +93,7 @@ class AdamW:
                 t.record_stream(s)
 
     def _clip(self, clip) -> int:
-        return self._clip_ptr if clip is self.clip else _ptr(clip, (torch.float32,), 2, "clip")
+        return self._clip_ptr if clip is self.clip else _ptr(clip, (torch.float32,), 2, "clip", self.device)
 
     # ---- setup
     def state_bytes(self) -> int:
@@ -102,28 +104,28 @@ class AdamW:
     def bind(self, params=None, copies=None, device=None, stream=None):
         """A new state block with zero moments; gradients have to be set again."""
         if device is None:
-            device = params[0].device if params else torch.device("cuda", torch.cuda.current_device())
-        self.device = torch.device(device)
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
+            device = next((t.device for t in params or () if t is not None), "cuda")
+        device = torch.device(device)
+        if device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
 
         def addresses(ts, dtype, what):
             if ts is None:
                 return None
             if len(ts) != len(self.shapes):
                 raise ValueError(f"expected {len(self.shapes)} {what}s, got {len(ts)}")
-            return (C.c_void_p * len(ts))(*[None if t is None else _ptr(t, (dtype,), k, what)
+            return (C.c_void_p * len(ts))(*[None if t is None else _ptr(t, (dtype,), k, what, device)
                                             for t, k in zip(ts, self.numels)])
 
         p, c = addresses(params, torch.float32, "parameter"), addresses(copies, torch.bfloat16, "copy")
-        on = torch.cuda.current_stream(self.device) if stream is None else stream
-        with torch.cuda.stream(on), torch.cuda.device(self.device):
+        on = torch.cuda.current_stream(device) if stream is None else stream
+        with torch.cuda.stream(on), torch.cuda.device(device):
             nbytes = self.state_bytes()
-            clip = torch.zeros(2, device=self.device)
-            state = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            clip = torch.zeros(2, device=device)
+            state = torch.empty(nbytes, dtype=torch.uint8, device=device)
             self._check(self.lib.acp_adamw_bind(self.opt, state.data_ptr(), nbytes, p, c, on.cuda_stream),
                         "acp_adamw_bind")
-        self._record(state, clip)
+        self.device, self._streams = device, {}
         self.clip, self._clip_ptr = clip, clip.data_ptr()
         self.state, self.params, self.copies = state, params, copies
         self._grads = {}
@@ -162,10 +164,10 @@ class AdamW:
                     raise ValueError("factors are matrices with one column per rank")
                 n = shape[0] if len(shape) > 1 else 1
                 x.rank = a.shape[1]
-                x.a = _ptr(a, (torch.float32,), n * x.rank, "factor")
-                x.b = _ptr(b, (torch.float32,), numel // n * x.rank, "factor")
+                x.a = _ptr(a, (torch.float32,), n * x.rank, "factor", self.device)
+                x.b = _ptr(b, (torch.float32,), numel // n * x.rank, "factor", self.device)
             else:
-                x.grad = _ptr(g, (torch.float32, torch.bfloat16), numel, "gradient")
+                x.grad = _ptr(g, (torch.float32, torch.bfloat16), numel, "gradient", self.device)
                 x.type = L.ACP_GRAD_BF16 if g.dtype == torch.bfloat16 else L.ACP_GRAD_FP32
         v = C.c_int64()
         self._check(self.lib.acp_adamw_grads_bytes(self.opt, arr, C.byref(v)), "acp_adamw_grads_bytes")
