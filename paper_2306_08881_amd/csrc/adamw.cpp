@@ -47,20 +47,22 @@ acp_status fail(const acp_adamw* o, acp_status s, const std::string& msg) {
   if (o) o->err = msg;
   return s;
 }
+// The same of a fixed text, also when the host has no memory for it (the last error then stays).
+acp_status fail(const acp_adamw* o, acp_status s, const char* msg) noexcept {
+  try {
+    if (o) o->err = msg;
+  } catch (...) {
+  }
+  return s;
+}
 
 // No C++ exception leaves a C entry: what is left to throw is the host's memory running out.
 template <class F>
 acp_status guarded(const acp_adamw* o, F f) {
   try {
     return f();
-  } catch (const std::bad_alloc&) {
-    try {
-      return fail(o, ACP_E_STATE, "out of host memory");
-    } catch (...) {
-      return ACP_E_STATE;
-    }
   } catch (...) {
-    return ACP_E_STATE;
+    return fail(o, ACP_E_STATE, "out of host memory");
   }
 }
 

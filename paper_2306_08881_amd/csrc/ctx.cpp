@@ -87,6 +87,24 @@ acp_status fail(const acp_ctx* c, acp_status s, const std::string& msg) {
   if (c) c->err = msg;
   return s;
 }
+// The same of a fixed text, also when the host has no memory for it (the last error then stays).
+acp_status fail(const acp_ctx* c, acp_status s, const char* msg) noexcept {
+  try {
+    if (c) c->err = msg;
+  } catch (...) {
+  }
+  return s;
+}
+
+// No C++ exception leaves a C entry: what is left to throw is the host's memory running out.
+template <class F>
+acp_status guarded(const acp_ctx* c, F f) {
+  try {
+    return f();
+  } catch (...) {
+    return fail(c, ACP_E_STATE, "out of host memory");
+  }
+}
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -976,44 +994,48 @@ acp_status acp_powersgd_decompress_all(acp_ctx* c, int64_t step, const float* co
 
 acp_status acp_advance(acp_ctx* c, int64_t step, int32_t b, const float* agg_factor, void* stream) {
   if (!c) return ACP_E_INVALID;
-  acp_status st = advance_ready(c, step, b);
-  if (st != ACP_OK) return st;
-  if (!agg_factor) return fail(c, ACP_E_INVALID, "null buffer");
-  if (!aligned16(agg_factor)) return fail(c, ACP_E_INVALID, "buffers must be 16-byte aligned");
-  if ((st = check_device(c)) != ACP_OK) return st;
-  acp::KArgs a = base_args(c);
-  a.base = b;
-  a.src[0] = agg_factor;
-  const int32_t parity = advance_parity(c, step, a);
-  RunOpts o;
-  o.skip_chol = c->plan.psgd;
-  if ((st = run(c, c->plan.buckets[b].advance[parity], a, static_cast<hipStream_t>(stream), o)) != ACP_OK) return st;
-  advanced(c, step, b);
-  return ACP_OK;
+  return guarded(c, [&]() -> acp_status {
+    acp_status st = advance_ready(c, step, b);
+    if (st != ACP_OK) return st;
+    if (!agg_factor) return fail(c, ACP_E_INVALID, "null buffer");
+    if (!aligned16(agg_factor)) return fail(c, ACP_E_INVALID, "buffers must be 16-byte aligned");
+    if ((st = check_device(c)) != ACP_OK) return st;
+    acp::KArgs a = base_args(c);
+    a.base = b;
+    a.src[0] = agg_factor;
+    const int32_t parity = advance_parity(c, step, a);
+    RunOpts o;
+    o.skip_chol = c->plan.psgd;
+    if ((st = run(c, c->plan.buckets[b].advance[parity], a, static_cast<hipStream_t>(stream), o)) != ACP_OK) return st;
+    advanced(c, step, b);
+    return ACP_OK;
+  });
 }
 
 acp_status acp_advance_all(acp_ctx* c, int64_t step, const float* const* agg_factors, void* stream) {
   if (!c) return ACP_E_INVALID;
-  if (!agg_factors) return fail(c, ACP_E_INVALID, "null pointer array");
-  const int32_t nb = static_cast<int32_t>(c->plan.buckets.size());
-  acp_status st = ACP_OK;
-  for (int32_t b = 0; b < nb; ++b) {
-    if ((st = advance_ready(c, step, b)) != ACP_OK) return st;
-    if (!agg_factors[b]) return fail(c, ACP_E_INVALID, "null buffer");
-    if (!aligned16(agg_factors[b])) return fail(c, ACP_E_INVALID, "buffers must be 16-byte aligned");
-  }
-  if ((st = check_device(c)) != ACP_OK) return st;
-  for (size_t g = 0; g < c->plan.group_advance.size(); ++g) {
-    acp::KArgs a = base_args(c);
-    a.base = static_cast<int32_t>(g) * acp::kMaxGroup;
-    for (int32_t i = 0; i < acp::kMaxGroup && a.base + i < nb; ++i) a.src[i] = agg_factors[a.base + i];
-    const int32_t parity = advance_parity(c, step, a);
-    RunOpts o;
-    o.skip_chol = c->plan.psgd;
-    if ((st = run(c, c->plan.group_advance[g][parity], a, static_cast<hipStream_t>(stream), o)) != ACP_OK) return st;
-  }
-  for (int32_t b = 0; b < nb; ++b) advanced(c, step, b);
-  return ACP_OK;
+  return guarded(c, [&]() -> acp_status {
+    if (!agg_factors) return fail(c, ACP_E_INVALID, "null pointer array");
+    const int32_t nb = static_cast<int32_t>(c->plan.buckets.size());
+    acp_status st = ACP_OK;
+    for (int32_t b = 0; b < nb; ++b) {
+      if ((st = advance_ready(c, step, b)) != ACP_OK) return st;
+      if (!agg_factors[b]) return fail(c, ACP_E_INVALID, "null buffer");
+      if (!aligned16(agg_factors[b])) return fail(c, ACP_E_INVALID, "buffers must be 16-byte aligned");
+    }
+    if ((st = check_device(c)) != ACP_OK) return st;
+    for (size_t g = 0; g < c->plan.group_advance.size(); ++g) {
+      acp::KArgs a = base_args(c);
+      a.base = static_cast<int32_t>(g) * acp::kMaxGroup;
+      for (int32_t i = 0; i < acp::kMaxGroup && a.base + i < nb; ++i) a.src[i] = agg_factors[a.base + i];
+      const int32_t parity = advance_parity(c, step, a);
+      RunOpts o;
+      o.skip_chol = c->plan.psgd;
+      if ((st = run(c, c->plan.group_advance[g][parity], a, static_cast<hipStream_t>(stream), o)) != ACP_OK) return st;
+    }
+    for (int32_t b = 0; b < nb; ++b) advanced(c, step, b);
+    return ACP_OK;
+  });
 }
 
 acp_status acp_factor_address(const acp_ctx* c, int32_t tensor_id, int32_t which, int32_t parity, const float** out) {
