@@ -820,7 +820,7 @@ __device__ inline void load_columns(float (&x)[T], Rsrc r, uint32_t at, int left
 
 template <int T, bool DIAG>
 __device__ inline void gram_tile(const AwGrad& gr, const float* x, int rows, int bi, int bj, double* out) {
-    constexpr int U = T == 4 ? 8 : 16 / T;  // steps of four rows loaded at a time
+  constexpr int U = T == 4 ? 8 : 16 / T;  // steps of four rows loaded at a time
   const int r = gr.rank, l16 = tid() & 15, q = (tid() >> 4) & 3;
   // rows past the slice read as zero
   const Rsrc rs = tile_rsrc(x, 4u * rows * r);
@@ -883,10 +883,14 @@ __global__ __launch_bounds__(kAwBlock) void k_norm(AwNormArgs a) {
     const int rows = static_cast<int>(left < per ? left : per);
     const float* x = (side ? gr.b : gr.a) + row0 * gr.rank;
     double* out = a.gram + gr.gram[side] + tile.first * aw_gram_entries(gr.rank, T) + aw_gram_at(gr.rank, T, bi, bj);
-    if (bi == bj)
-      gram_tile<T, true>(gr, x, rows, bi, bj, out);
-    else
-      gram_tile<T, false>(gr, x, rows, bi, bj, out);
+    // (a block of fewer columns holds the slot's whole matrices)
+    if constexpr (T == 4) {
+      if (bi != bj) {
+        gram_tile<T, false>(gr, x, rows, bi, bj, out);
+        return;
+      }
+    }
+    gram_tile<T, true>(gr, x, rows, bi, bj, out);
   }
 }
 
