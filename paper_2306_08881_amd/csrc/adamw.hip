@@ -156,23 +156,25 @@ __device__ inline float root(float x) {
 // whole code now and then, which another program's replay of the step would see (fused and with the bare
 // instruction for the root: BERT-large rank 32 937 us, so 944).  p's quotient is m' times the hardware's
 // reciprocal (1 ulp; eps > 0 keeps the denominator a normal number, and an infinite one gives 0).
-// Subnormal v' are scaled for their roots, in waves that have any (BERT-large rank 32, 8 bits, 941 us without,
-// 949 so; 960 with every element scaled or not by a select, and BERT-base 340, 346 and 342).
-constexpr int kSubnormal = 0x80;  // class of positive subnormal numbers
+// Subnormal v' are scaled for their roots, in waves that have any (8 bits, BERT-base 341 us without, 347 so;
+// BERT-large rank 64 1016 and 1035, 256 2548 and 2536, others within 1 %; with every element scaled or not by a
+// select rank 4 744 and 760, rank 256 3093).  They are found by the least of the bits less one, where 0 counts as
+// large: a class test of each value took more scalar registers (rank 256 2805 us).
 __device__ inline void update4(const AwArgs& a, const Coef& k, const float (&g)[4], float (&p)[4], float (&m)[4],
                                float (&v)[4], float (&r)[4]) {
-  bool tiny = false;
+  uint32_t least = ~0u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float c = g[i] * k.c;
     m[i] = m[i] * a.b1 + c * a.c1;
     v[i] = v[i] * a.b2 + (c * c) * a.c2;
     r[i] = root(v[i]);
-    tiny = tiny || __builtin_amdgcn_classf(v[i], kSubnormal);
+    const uint32_t b = __builtin_bit_cast(uint32_t, v[i]) - 1u;
+    least = b < least ? b : least;
   }
-  if (__builtin_expect(__any(tiny), 0)) {
+  if (__builtin_expect(__any(least < 0x007FFFFFu), 0)) {  // (2^-126)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = v[i] < 0x1p-126f ? root(v[i] * 0x1p64f) * 0x1p-32f : r[i];
+    for (int i = 0; i < 4; ++i) r[i] = v[i] < 0x1p-126f ? __builtin_amdgcn_sqrtf(v[i] * 0x1p64f) * 0x1p-32f : r[i];
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
