@@ -1,0 +1,72 @@
+"""Steps that end with acp_advance among steps that end with acp_decompress: from rank 8 on only the latter forms
+the next step's orthogonal factor beside itself, and the next compress has to know which it was."""
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [(300, 200), (300,), (64, 3, 7, 7), (64,), (513, 270), (17, 1000), (2, 5), (1030, 520)]
+ENDS = "daadadda"  # per step: decompress or advance
+
+
+def run(rank, ends, per_bucket=False, powersgd=False, reuse=True):
+    """Factor buffers, M_hat where it is written, and the error after all steps.  ends(t, b): whether step t of
+    bucket b ends with advance."""
+    import torch
+    from paper_2306_08881_amd.acp import Acp
+    acp = Acp(SHAPES, rank, seed=3, cap_bytes=1 << 18, powersgd=powersgd, reuse=reuse)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    buckets = range(acp.num_buckets())
+    assert len(buckets) > 2
+    info = [acp.bucket_info(b) for b in buckets]
+    factors, hats = [], []
+    for t in range(1, len(ENDS) + 1):
+        grads = [torch.randn(i[1], generator=gen, device="cuda") for i in info]
+        p, q, hat = ([torch.zeros(i[k], device="cuda") for i in info] for k in (2, 3, 1))
+        agg = q if powersgd or t % 2 == 0 else p
+        if powersgd:
+            acp.powersgd_p_all(t, grads, p)
+            acp.powersgd_q_all(t, grads, p, q)
+        elif per_bucket:
+            for b in buckets:
+                acp.compress(t, b, grads[b], agg[b])
+        else:
+            acp.compress_all(t, grads, agg)
+        if per_bucket:
+            for b in buckets:
+                if ends(t, b):
+                    acp.advance(t, b, agg[b])
+                elif powersgd:
+                    acp.powersgd_decompress(t, b, agg[b], hat[b])
+                else:
+                    acp.decompress(t, b, agg[b], hat[b])
+        elif ends(t, 0):
+            acp.advance_all(t, agg)
+        elif powersgd:
+            acp.powersgd_decompress_all(t, agg, hat)
+        else:
+            acp.decompress_all(t, agg, hat)
+        factors.append(agg)
+        hats.append([None if ends(t, b if per_bucket else 0) else hat[b] for b in buckets])
+    errors = [torch.zeros(i[1], device="cuda") for i in info]
+    for b in buckets:
+        acp.error(b, errors[b])
+    torch.cuda.synchronize()
+    return factors, hats, errors
+
+
+KINDS = [dict(rank=r) for r in (1, 4, 8, 16, 32, 64, 128, 256)] + [dict(rank=16, powersgd=True), dict(rank=8, reuse=False)]
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=str)
+@pytest.mark.parametrize("per_bucket", [False, True])
+def test_mixed_ends(kind, per_bucket):
+    import torch
+    want = run(ends=lambda t, b: False, **kind)
+    for shift in (0, 1):  # both kinds at odd and at even steps, after either kind
+        got = run(ends=lambda t, b: ENDS[(t + b + 4 * shift) % len(ENDS)] == "a", per_bucket=per_bucket, **kind)
+        for t, (x, y) in enumerate(zip(want[0], got[0]), 1):
+            assert all(torch.equal(a, b) for a, b in zip(x, y)), f"factors of step {t}"
+        for t, (x, y) in enumerate(zip(want[1], got[1]), 1):
+            assert all(b is None or torch.equal(a, b) for a, b in zip(x, y)), f"M_hat of step {t}"
+        assert all(torch.equal(a, b) for a, b in zip(want[2], got[2]))
