@@ -392,7 +392,8 @@ void acp_destroy(acp_ctx *ctx);
  * Values are rounded up or down at random with the expected value kept (a moment moves by less than a
  * rounding step at a time, which rounding to nearest would lose), by a hash of seed, step, tensor and
  * element: the same calls give the same bits.  sqrt(v) > 0 is not rounded to 0.  A block whose largest
- * magnitude is below 2^-100 becomes zero, one with a value that is not finite becomes NaN as a whole.
+ * magnitude is below 2^-100 becomes zero, one with a value that is not finite, or above 2^126 in magnitude,
+ * becomes NaN as a whole.
  *
  * Ownership: the caller owns every device buffer and stream; nothing is allocated on the device.
  * acp_adamw_norm and acp_adamw_step enqueue kernels only and may be captured into a HIP graph, with the
@@ -456,8 +457,9 @@ acp_status acp_adamw_tensor_info(const acp_adamw *opt, int32_t tensor, int64_t *
  * whose gradients alternate between buffers (the compressor's factors swap roles with the step's
  * parity) sets a slot for each once and names it in every call.  The device block (256-byte aligned, of
  * acp_adamw_grads_bytes for the same entries) takes the launch tables and the norm's partial sums and
- * belongs to the slot until it is set again, or the state bound again; so do the gradients' places.  Uploads
- * on `stream` and waits for it.  Factors may be read-only views of a context's state
+ * belongs to the slot until it is set again, or the state bound again; so do the gradients' places.  Plans
+ * all tiles on the host (1 to 4 ms for 334 M elements: more than a step takes, so set what stays in place once),
+ * uploads them on `stream` and waits for it.  Factors may be read-only views of a context's state
  * (acp_factor_address).  ACP_E_INVALID if a gradient overlaps what the calls write (the state, parameters and
  * copies, any slot's block) or the block any of these or any slot's gradients; also, from acp_adamw_grads_bytes
  * on, for 2^22 tiles of a kind or more (the launches' limit; take several optimisers).  A tile is, of a
@@ -474,8 +476,8 @@ acp_status acp_adamw_set_grads(acp_adamw *opt, int32_t slot, const acp_adamw_gra
  * acp_adamw_norm - the 2-norm of `scale` times all gradients of a slot together, and the coefficient
  * that clips it: clip[0] = norm, clip[1] = min(1, max_norm / norm), NaN if the norm is not finite (clip:
  * device, two floats; ACP_E_INVALID if they overlap the state, parameters, copies or a slot's block or
- * gradients).  Sums are in fp64 in a fixed order.  A factored gradient's part is
- * sum (a^T a) o (b^T b).  max_norm > 0; infinity does not clip.
+ * gradients).  Sums are in fp64 in a fixed order; the squares of two bfloat16 values are added in fp32 first
+ * (at most 2^-25 of the norm).  A factored gradient's part is sum (a^T a) o (b^T b).  max_norm > 0; infinity does not clip.
  */
 acp_status acp_adamw_norm(acp_adamw *opt, int32_t slot, float scale, float max_norm, float *clip, void *stream);
 

@@ -185,6 +185,7 @@ __device__ inline void update4(const AwArgs& a, const Coef& k, const float (&g)[
 
 // ---- 8-bit moments -----------------------------------------------------------------------------
 
+// The 32-bit finaliser of MurmurHash3 (A. Appleby, public domain).
 __device__ inline uint32_t mix32(uint32_t x) {
   x ^= x >> 16;
   x *= 0x85EBCA6Bu;
@@ -195,7 +196,10 @@ __device__ inline uint32_t mix32(uint32_t x) {
 __device__ inline uint32_t tensor_key(uint32_t key, int tensor) {
   return mix32(key + static_cast<uint32_t>(tensor) * 0x9E3779B1u);
 }
-// 32 random bits of element e, x = key + e * kElementStep (elements 2^32 apart share theirs)
+// 32 random bits of element e, x = key + e * kElementStep (elements 2^32 apart share theirs).  Shifts and
+// multiplier are those of the first of two rounds of a published integer hash; one round, for its price (of 56
+// vector instructions an element 11 are the rounding's).  What it has to do is to leave the mean of the rounding's
+// errors at zero, over elements and over steps.
 constexpr uint32_t kElementStep = 0x9E3779B1u;
 __device__ inline uint32_t random_bits(uint32_t x) {
   x ^= x >> 15;
@@ -464,9 +468,9 @@ constexpr int product_group(int kc) { return aw_product_waves(16 * kc); }
 // The operands of a product for 16 rows of A or B, 16 KC values of the inner dimension, row l of a factor's
 // rows in `r` from value `row` on: lane 16 q + l has the values 4 q .. 4 q + 3 of each 16, or below rank 16 the
 // values 4 s + q, so that whole steps of four can be left out; at rank 16 the values 2 q, 2 q + 1 of each 8.
-// Values from `rank` on, and of rows past the end, are zero.  Any of these orders will do; these are the ones
-// in which the library's fp32 product adds up at ranks up to 16, at 32 and for many matrices above, so that
-// a program which forms A B^T there and steps on its values gets the same codes.
+// Values from `rank` on, and of rows past the end, are zero.  Any order of the sum would do for its error bound; with
+// these, sums over ranks up to 16 and of 32 came out bit for bit as those of the BLAS library that this was
+// measured beside, which says nothing of another version of it.
 template <int KC>
 __device__ inline void load_operand(f4 (&x)[KC], Rsrc r, uint32_t row, int q, int rank) {
   if (KC == 1 && rank == 16) {
@@ -523,12 +527,13 @@ __device__ inline void multiply(f4 (&acc)[J], const f4 (&a)[KC], const f4 (&b)[J
 // The product of the next 16 rows runs beside the step of these, and the next row's state is requested as
 // soon as a row is done.
 //
-// BERT-large: 32 bits, rank 4, 24 bytes an element, 1295 us, 6.2 TB/s: HBM.  8 bits, 12.1 bytes: rank 4 715 us
-// (with 5.6 TB/s), rank 32 and a bfloat16 copy 880 us (5.3 TB/s): the vector units (71 % busy), which share
-// their SIMD with the matrix cores' turns and the barriers.  Rank 64 1000 us, 128 1365 us, 256 2540 us: the
+// BERT-large: 32 bits, rank 4, 24 bytes an element, 1277 us, 6.3 TB/s: HBM.  8 bits, 12.1 bytes: rank 4 718 us
+// (5.6 TB/s), rank 32 814 and with a bfloat16 copy 870 us (5.4 TB/s): the vector units (74 % busy), which share
+// their SIMD with the matrix cores' turns and the barriers.  Rank 64 1012 us, 128 1362 us, 256 2530 us: the
 // fp32 matrix cores (for which alone 272, 544 and 1088 us are needed) and the few waves that B's registers
-// leave.  Decompressing first and stepping on values takes 1084 us at rank 4, 1299 at rank 32, 1794 at rank 128
-// and 3069 at rank 256, of which advancing without M_hat's values leaves 30, 60, 290 and 860.
+// leave.  With 32 bits a tile has one group of 16 rows, whose product nothing runs beside: rank 64 1555 us, 128
+// 2228, 256 4895.  A whole step from the compress call on, 8 bits, with M_hat written and without: rank 4 1739 and
+// 1397 us, rank 32 1909 and 1610, rank 64 2171 and 2083, rank 128 3085 and 3250, rank 256 5834 and 7034.
 template <int BITS, int KC, bool WIDE>
 __device__ inline void product_rows(const AwArgs& a, const AwTensor& t, const AwTile& tile, const Coef& k,
                                     const AwGrad& gr, float (*lds)[kAwRows * kLdsPitch]) {
@@ -727,8 +732,8 @@ __device__ inline double block_sum(double v) {
 
 // Squares and their sums are in 64 bits: no finite gradient overflows, and the result does not
 // depend on how the tiles are cut beyond its last bits.  bfloat16 values' squares are exact in fp32
-// where they are normal numbers there; two of them are added in fp32 before they go on in 64 bits, unless the
-// wave has values too large or small for that (BERT-large, eight bytes
+// where they are normal numbers there; two of them are added in fp32 (2^-24 of their sum at most, 2^-25 of the norm)
+// before they go on in 64 bits, unless the wave has values too large or small for that (BERT-large, eight bytes
 // a load: 133 us with every square in 64 bits, 121 so). A lane loads 16 bytes of either type: bfloat16 103 us
 // (6.5 TB/s), 121 with eight; fp32 197 us (6.8 TB/s). HBM bounds both.
 __device__ inline void norm_tile(const AwNormArgs& a, const AwTile& tile, double* out) {
@@ -803,7 +808,8 @@ __device__ inline void norm_tile(const AwNormArgs& a, const AwTile& tile, double
 // long as A and B have the same.  Slices of 256 rows: longer ones leave CUs idle, shorter ones
 // write more partial sums (rank 4: 36 us with 256 rows, 39 with 512, 41 with 128).
 // BERT-large rank 64: 76 us of the norm's 92, a third of the fp64 matrix cores' peak: one wave per SIMD, for
-// the loads in flight that the registers hold.
+// the registers of the blocks off the diagonal (368), which ranks above 64 have, in the same kernel.  Rank 256: 964 us
+// in all.
 template <int T>
 __device__ inline void load_columns(float (&x)[T], Rsrc r, uint32_t at, int left) {
   if (left >= T) {

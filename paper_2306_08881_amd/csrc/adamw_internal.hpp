@@ -29,19 +29,30 @@ constexpr int kAwPart = 256;            // elements a wave takes of a dense tile
 constexpr int kAwPartBlocks = 2;        // blocks it takes (8-bit moments, rows of whole words)
 constexpr int64_t kAwTile = 2048;       // elements of a dense tile
 constexpr int64_t kAwTileBlocks = 16;   // blocks of one
-// Elements of a tile of the norm: longer ones where there are enough (BERT-large, bfloat16, 127 us with
-// 16384 and 120 with 32768; ResNet-50 19.3 and 20.1)
+// Elements of a tile of the norm: longer ones where the optimiser has enough elements.  us with 16384 and 32768,
+// one tensor of values: fp32 8 M elements 9.3 and 10.5, 32 M 23.0 and 24.1, 64 M 43.1 and 43.7, 128 M 82.4 and
+// 82.3, 512 M 319 and 312; bfloat16 8 M 8.2 and 9.0, 32 M 14.5 and 14.5, 64 M 24.5 and 24.0, 512 M 168 and 162.
 constexpr int64_t aw_norm_tile(int64_t elems) { return elems >= int64_t(1) << 26 ? 32768 : 16384; }
 constexpr int kAwRows = 16;             // rows of A B^T that go through LDS at a time
 // Groups of kAwRows rows that a tile of A B^T has, at most: its wave loads B's part once for them.  They
 // lie as many groups apart as there are tiles in the column, so that all workgroups together sweep
-// through the tensor in step (8 bits, BERT-large rank 32: neighbouring groups 1116 us, these 1055).  With 32
-// bits HBM is what counts, and one group is best (rank 4: 1450 us with two, 1390 with one).  A slot with few
-// groups has fewer a tile, so that there are kAwProductTiles tiles.
+// through the tensor in step (8 bits, BERT-large rank 32: neighbouring groups 1116 us, these 1055).
+// BERT-large, us with 1, 2, 4 and 16 groups:
+//   8 bits   rank 4   794  735  718  779     rank 32   974  856  814  811     rank 64 1452 1243 1117 1012
+//            rank 128 2284 1782 1581 1362    rank 256 5305 3886 3086 2528
+//   32 bits  rank 4  1277 1327 1427 1511     rank 16  1327 1324 1416 1511     rank 32 1308 1357 1410 1513
+//            rank 64 1555 1428 1428 1492     rank 128 2228 1848 1670 1573     rank 256 4895 3652 3161 2824
+// With 32 bits HBM is what counts up to rank 32, and one group is best.  Above, B's part, loaded for 16 rows only,
+// costs more than that gains: there the rule for 32 bits is not the best one.
+// A slot with few groups has fewer a tile, so that there are kAwProductTiles tiles: 8 bits, us with 1024, 2048,
+// 4096 and 8192, BERT-base rank 32 272 272 272 277, rank 64 366 354 363 381, rank 128 484 473 497 531,
+// ResNet-50 rank 4 67.5 66.3 66.7 66.8, rank 64 104 107 121 121.
 constexpr int aw_row_groups(int bits, int rank) { return bits == 32 ? 1 : rank <= 32 ? 4 : 16; }
 constexpr int64_t kAwProductTiles = 4096;
 // Dense tensors beside factored ones go with the products' launch up to this many elements (the vectors of a
-// model, or what else a launch of its own, 5 us, would cost more than their lower occupancy there)
+// model, or what else a launch of its own would cost more than their lower occupancy there).  us in their launch and
+// in one of their own, beside factors of 4096 x 4096: 8 bits 64 K elements 45.3 and 49.1, 1 M 48.4 and 50.9, 2 M
+// 52.1 and 52.9, 8 M 69.5 and 70.1; 32 bits 64 K 67.1 and 69.6, 2 M 76.6 and 78.7, 8 M 102.6 and 105.0.
 constexpr int64_t kAwJoined = int64_t(1) << 21;
 
 // Waves of a workgroup of A B^T that share a tile's columns: four, which meet at fewer barriers (8 bits, BERT-large
