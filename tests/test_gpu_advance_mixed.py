@@ -70,3 +70,36 @@ def test_mixed_ends(kind, per_bucket):
         for t, (x, y) in enumerate(zip(want[1], got[1]), 1):
             assert all(b is None or torch.equal(a, b) for a, b in zip(x, y)), f"M_hat of step {t}"
         assert all(torch.equal(a, b) for a, b in zip(want[2], got[2]))
+
+
+@pytest.mark.parametrize("rank", [4, 8, 64, 256])
+@pytest.mark.parametrize("steps", [1, 2, 3])
+def test_checkpoint_after_advance(rank, steps):
+    """A state saved after steps that ended with advance continues, restored, with the same bits."""
+    import torch
+    from paper_2306_08881_amd.acp import Acp
+
+    def go(acp, first, last, end):
+        info = [acp.bucket_info(b) for b in range(acp.num_buckets())]
+        out = []
+        for t in range(first, last + 1):
+            gen = torch.Generator(device="cuda").manual_seed(t)
+            grads = [torch.randn(i[1], generator=gen, device="cuda") for i in info]
+            agg, hat = ([torch.zeros(i[k], device="cuda") for i in info] for k in (2 if t % 2 else 3, 1))
+            acp.compress_all(t, grads, agg)
+            if end == "a":
+                acp.advance_all(t, agg)
+            else:
+                acp.decompress_all(t, agg, hat)
+                out += hat
+            out += agg
+        torch.cuda.synchronize()
+        return out
+
+    x, y, z = (Acp(SHAPES, rank, seed=3, cap_bytes=1 << 18) for _ in range(3))
+    go(x, 1, steps, "a")
+    go(z, 1, steps, "d")
+    y.set_state(x.get_state())
+    want = go(z, steps + 1, steps + 3, "d")
+    for acp in (x, y):
+        assert all(torch.equal(a, b) for a, b in zip(want, go(acp, steps + 1, steps + 3, "d")))
